@@ -187,7 +187,9 @@ extern "C" int sp_pruned_decode_tree(const void *q, const void *k_cache, const v
     SP_REQUIRE(aligned16(q) && aligned16(out) && aligned16(k_cache) && aligned16(v_cache) && aligned16(tail_k) && aligned16(tail_v),
                SP_ERR_INVALID_ARG, "sp_pruned_decode_tree: data pointers must be 16-byte aligned");
     const int64_t bound = (int64_t)lay->max_pre_len + (int64_t)k * lay->max_path_len + tail_cap;
-    SP_REQUIRE(bound < (int64_t)INT32_MAX - 256, SP_ERR_UNSUPPORTED, "sp_pruned_decode_tree: up to %lld keys per prompt", (long long)bound);
+    // Numbers of keys are 32 bits: with the gaps that TreeTable leaves in front of multiples of kTtPad, and what a tile reaches behind the last one.
+    const int64_t numbers = bound + (dtype == SP_BF16 ? (int64_t)(kTtPad - 1) * (k + 1) : 0);
+    SP_REQUIRE(numbers < (int64_t)INT32_MAX - 256, SP_ERR_UNSUPPORTED, "sp_pruned_decode_tree: up to %lld keys per prompt", (long long)bound);
     SP_REQUIRE(ws && aligned256(ws) && ws_bytes >= sp_decode_tree_workspace_bytes(lay->n_prompts, max_nodes, n_heads, head_dim), SP_ERR_WORKSPACE,
                "sp_pruned_decode_tree: workspace of %zu bytes (256-byte aligned) required", sp_decode_tree_workspace_bytes(lay->n_prompts, max_nodes, n_heads, head_dim));
 

@@ -10,6 +10,7 @@
 namespace sp {
 
 constexpr int kTreeMaxNodes = 64;                // a node's ancestors are the bits of one 64-bit word
+constexpr int kTtPad = 8;                        // the bf16 kernel's segments start at multiples of this: the smallest TMA box's rows
 constexpr float kLog2eT = 1.4426950408889634f;
 constexpr float kLn2T = 0.6931471805599453f;
 

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kTtThreads, 2) tree_tc_kernel(const __grid_con
     // blocks of this kernel fit on an SM, whose 512 columns are enough for both.
     if (warp == kTtMmaWarp) { tmem_alloc(&sh.tmem, kTtTmem); tmem_relinquish(); }
     tc_fence_before();
-    const bool some = table.fill(a, b, 8);       // the same for all blocks of the cluster, as is rows; two barriers, behind which barriers and tensor memory are everybody's
+    const bool some = table.fill(a, b, kTtPad);       // the same for all blocks of the cluster, as is rows; two barriers, behind which barriers and tensor memory are everybody's
     const int group = a.n_heads / a.n_kv_heads, rows = some ? min(table.head->n * group - first_row, p.tile_rows) : 0;
     if (rows <= 0) {
         if (warp == kTtMmaWarp) tmem_dealloc(sh.tmem, kTtTmem);

@@ -35,6 +35,18 @@ def test_tree_refusals(change, code, text):
     assert text in sp.lib.sp_last_error().decode()
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_tree_key_numbers_stay_below_2_31(dtype):
+    """bf16 numbers keys from multiples of eight in every segment: up to seven numbers a segment that stand for no key count too.  (A path may be kept
+    several times, so that this takes no 2^31 rows.)  The workspace is looked at behind the number of keys: without one nothing is launched."""
+    k, pre, path = 4096, 2, 524272
+    lay = sp.binding._CLayout(1, 1, P, P, P, P, P, P, 600000, pre, path)
+    call = lambda cap: sp.lib.sp_pruned_decode_tree(*_tree_args(lay=ctypes.byref(lay), k=k, tail_cap=cap, ws=None, dtype=dtype)[0])
+    most = 2 ** 31 - 1 - 256 - (pre + k * path) - (7 * (k + 1) if dtype else 0) - 1         # rows of the tail that are still fine
+    assert call(most) == sp.SP_ERR_WORKSPACE
+    assert call(most + 1) == sp.SP_ERR_UNSUPPORTED and "keys" in sp.lib.sp_last_error().decode()
+
+
 def test_nothing_to_do_is_fine():
     assert sp.lib.sp_pruned_decode_tree(*_tree_args(max_nodes=0)[0]) == sp.SP_OK
     assert sp.lib.sp_sample_tokens(None, 8, 0, 8, None, None, None, None, None, None, None, 0, None) == sp.SP_OK
