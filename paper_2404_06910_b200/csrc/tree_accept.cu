@@ -120,7 +120,8 @@ extern "C" int sp_tree_accept(const int32_t *draft, const int32_t *sampled, cons
     a.path = path; a.n_accepted = n_accepted; a.next_token = next_token; a.new_tail_len = new_tail_len;
     a.tail_k = static_cast<unsigned char *>(tail_k); a.tail_v = static_cast<unsigned char *>(tail_v);
     a.layer_bytes = ld_layer * elt_bytes(dtype);
-    a.max_nodes = max_nodes; a.tail_cap = tail_cap; a.n_layers = n_layers; a.row_vecs = (int)(row_bytes / 16);
+    a.max_nodes = max_nodes; a.n_layers = n_layers; a.row_vecs = (int)(row_bytes / 16);
+    a.tail_cap = n_layers > 0 ? tail_cap : INT32_MAX;       // lengths alone need no room, but have to stay numbers
     // a column per thread, as far as eight blocks per SM go
     const int64_t columns = 2LL * n_layers * a.row_vecs, want = (columns + kAccThreads - 1) / kAccThreads;
     const int64_t most = std::max<int64_t>(1, 8LL * num_sms() / n_prompts);
