@@ -367,11 +367,20 @@ def sp_sample_tokens(logits, u, tokens, logp=None, *, temperature=None, top_k=No
 def sp_tree_accept(draft, sampled, parent, n_nodes, path, n_accepted, next_token, tail_k=None, tail_v=None,
                    tail_len=None, new_tail_len=None, stream=None):
     """The walk down a tree of drafts (draft, sampled, parent int32 [B, N]) and the compaction of the tails
-    [n_layers, B, cap, Hkv, D] in place."""
+    [n_layers, slots, cap, Hkv, D] in place; prompt b has slot b, of B or more."""
     B, N = parent.shape
-    L, _, cap, Hkv, D = (0, 0, 0, 0, 0) if tail_k is None else tail_k.shape
+    L, cap, ld, Hkv, D, dtype = 0, 0, 0, 0, 0, SP_F32
+    if (tail_k is None) != (tail_v is None):
+        raise ValueError("tail_k and tail_v come together")
+    if tail_k is not None:
+        if tail_v.shape != tail_k.shape or tail_v.dtype != tail_k.dtype:
+            raise ValueError("tail_k and tail_v must have one shape and type")
+        L, slots, cap, Hkv, D = tail_k.shape
+        if slots < B:
+            raise ValueError(f"tails of {slots} slots for {B} prompts")
+        ld, dtype = tail_k.stride(0), dtype_code(tail_k)
     _call(_ACCEPT, draft, sampled, parent, n_nodes, B, N, path, n_accepted, next_token, tail_k, tail_v, tail_len,
-          new_tail_len, cap, L, B * cap * Hkv * D, Hkv, D, SP_F32 if tail_k is None else dtype_code(tail_k), _stream(stream))
+          new_tail_len, cap, L, ld, Hkv, D, dtype, _stream(stream))
 
 
 def sp_check_status(ws, stream=None) -> None:

@@ -1,8 +1,10 @@
 """Speculative decoding, host side: refusals of the three entry points (all before any launch) and the plain forms against each other."""
 import ctypes
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2404_06910_b200 as sp
 import spec_reference as ref
@@ -78,6 +80,19 @@ def test_accept_refusals(change, code, text):
     a.update(change)
     assert sp.lib.sp_tree_accept(*a.values()) == getattr(sp, "SP_ERR_" + code)
     assert text in sp.lib.sp_last_error().decode()
+
+
+@pytest.mark.parametrize("k,v,text", [
+    ((2, 2, 8, 2, 64), None, "come together"), (None, (2, 2, 8, 2, 64), "come together"),
+    ((2, 1, 8, 2, 64), (2, 1, 8, 2, 64), "slots"), ((2, 2, 8, 2, 64), (2, 2, 7, 2, 64), "shape"), ((2, 2, 8, 2, 64), (1, 2, 8, 2, 64), "shape"),
+    ((2, 2, 8, 2, 64), (2, 2, 8, 2, 128), "shape"), ((2, 2, 8, 2, 64), "bf16", "shape")])
+def test_accept_takes_tails_alike_with_a_slot_for_every_prompt(k, v, text):
+    """What the C entry point cannot see: refused before any launch."""
+    make = lambda s, dtype=torch.float32: None if s is None else torch.zeros(s, dtype=dtype)
+    tree, one = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match=text):
+        sp.sp_tree_accept(tree, tree, tree, one, tree, one, one, make(k), make(k, torch.bfloat16) if v == "bf16" else make(v), one, one,
+                          stream=SimpleNamespace(cuda_stream=0))
 
 
 def test_plain_tree_of_a_chain_is_causal_attention():
