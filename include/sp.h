@@ -371,7 +371,8 @@ int sp_sample_tokens(const void *logits, int64_t ld_logits, int64_t n_rows, int 
  * ld_layer elements, are compacted in place: row tail_len[b] + j becomes row tail_len[b] + path[b][j]; rows behind
  * new_tail_len[b] = tail_len[b] + n_accepted[b] are the rejected nodes' and may be written over.  n_layers 0: no
  * tails (NULL; tail_cap is not looked at, any tail_len >= 0 will do), and tail_len / new_tail_len NULL or both given.
- * A prompt whose n_nodes or tail_len is impossible (see above) accepts nothing.  Outputs must not overlap inputs (new_tail_len is not tail_len).  No workspace.
+ * A prompt whose n_nodes or tail_len is impossible (see above) accepts nothing.  Outputs must not overlap inputs
+ * (new_tail_len is not tail_len), nor K tails V tails.  No workspace.
  */
 int sp_tree_accept(const int32_t *draft, const int32_t *sampled, const int32_t *parent, const int32_t *n_nodes,
                    int n_prompts, int max_nodes, int32_t *path, int32_t *n_accepted, int32_t *next_token,

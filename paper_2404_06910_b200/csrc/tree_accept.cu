@@ -5,6 +5,8 @@
 // ballot per step) and then moves its share of the columns.  A thread owns 16 bytes of a row and takes the moves in ascending order, four loads
 // before four stores: node j of the path goes to row j <= its own, so what a store overwrites has been read, by the same thread.
 // 64 prompts x 32 nodes, 16 layers of 8 x 128: 5.3 us, of which launch and the walk's dependent loads are all but 1.6 (the moved rows' bytes).
+#include <cstdlib>
+
 #include "common.cuh"
 
 namespace sp {
@@ -105,6 +107,13 @@ extern "C" int sp_tree_accept(const int32_t *draft, const int32_t *sampled, cons
         SP_REQUIRE(aligned16(tail_k) && aligned16(tail_v), SP_ERR_INVALID_ARG, "sp_tree_accept: tails must be 16-byte aligned");
         SP_REQUIRE(n_layers == 1 || (ld_layer >= (int64_t)n_prompts * tail_cap * n_kv_heads * head_dim && ld_layer * elt_bytes(dtype) % 16 == 0),
                    SP_ERR_INVALID_ARG, "sp_tree_accept: ld_layer %lld is too small or not a multiple of 16 bytes", (long long)ld_layer);
+        // K and V of two layers l and m lie |d + (m - l) stride| apart: of the differences m - l the two nearest to -d / stride
+        const int64_t size = (int64_t)n_prompts * tail_cap * row_bytes, stride = n_layers > 1 ? ld_layer * elt_bytes(dtype) : 0;
+        const int64_t d = static_cast<char *>(tail_v) - static_cast<char *>(tail_k);
+        bool apart = stride || std::abs(d) >= size;
+        for (int64_t j = stride ? d / stride - 1 : 0; stride && j <= d / stride + 1; ++j)
+            apart &= std::abs(j) >= n_layers || std::abs(d - j * stride) >= size;
+        SP_REQUIRE(apart, SP_ERR_INVALID_ARG, "sp_tree_accept: the K and V tails overlap");
     }
     // every block reads the inputs and one writes the outputs
     const struct { const void *p; int64_t n; } in[] = {{draft, max_nodes}, {sampled, max_nodes}, {parent, max_nodes}, {n_nodes, 1}, {tail_len, 1}},

@@ -95,6 +95,20 @@ def test_accept_takes_tails_alike_with_a_slot_for_every_prompt(k, v, text):
                           stream=SimpleNamespace(cuda_stream=0))
 
 
+@pytest.mark.parametrize("layers,ld,away,apart", [
+    (1, 0, 0, False), (1, 0, 4095, False), (1, 0, 4096, True), (1, 0, -4095, False), (1, 0, -4096, True),       # elements from the K to the V tail; a layer is 4096
+    (3, 4096, 4096, False), (3, 4096, 2 * 4096, False), (3, 4096, 3 * 4096, True), (3, 4096, -2 * 4096, False), (3, 4096, -3 * 4096, True),
+    (3, 8192, 4096, True), (3, 8192, 4092, False), (3, 8192, -4096, True), (3, 8192, -4100, False), (3, 10000, 4096, True), (3, 10000, 5904, True), (3, 10000, 5908, False),
+    (3, 8192, 5 * 4096, True), (3, 8192, 4 * 4096, False), (3, 8192, 6 * 4096, True)])
+def test_accept_refuses_k_and_v_tails_that_overlap(layers, ld, away, apart):
+    """Two threads would move the same rows.  Tails that lie between one another (a layer's K, its V, the next layer's K) are fine: they get as far as
+    the check of the outputs, which overlap an input here, so that nothing is launched."""
+    at, away = 16 * P, away // 4 * 4 if away >= 0 else -(-away // 4 * 4)
+    code = sp.lib.sp_tree_accept(P, P + 4096, P + 2 * 4096, None, 2, 4, P + 16, 2 * P, 3 * P, at, at + 4 * away, P + 4 * 4096, 4 * P, 16, layers, ld, 2, 64, 0, None)
+    assert code == sp.SP_ERR_INVALID_ARG
+    assert ("outputs" if apart else "tails overlap") in sp.lib.sp_last_error().decode()
+
+
 def test_plain_tree_of_a_chain_is_causal_attention():
     """In the plain form a chain behind a context is causal attention over the concatenation."""
     rng = np.random.default_rng(0)
