@@ -243,7 +243,8 @@ __device__ __forceinline__ void tree_merge(const TreeArgs &a, float *part, int r
             x.load<COPIES>([&](int j) { return part + (r + j * (128 / COPIES)) * PS; }, c, D);
             x.join<COPIES>();
             if (n == 1) { write(x, r, c); continue; }
-            __syncwarp(__activemask());          // all pieces' threads have read reference and sum
+            // all pieces' threads have read reference and sum: a row's are 16 or 32 neighbouring lanes, all of which are here
+            __syncwarp(PIECES == 32 ? 0xffffffffu : 0xffffu << (threadIdx.x & 16));
             float *p = part + r * PS;
             *reinterpret_cast<float4 *>(p + c) = make_float4(x.o[0], x.o[1], x.o[2], x.o[3]);
             if (c == 0) { p[D] = x.m; p[D + 1] = x.l; }

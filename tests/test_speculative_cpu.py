@@ -1,5 +1,6 @@
 """Speculative decoding, host side: refusals of the three entry points (all before any launch) and the plain forms against each other."""
 import ctypes
+import pathlib
 from types import SimpleNamespace
 
 import numpy as np
@@ -107,6 +108,12 @@ def test_accept_refuses_k_and_v_tails_that_overlap(layers, ld, away, apart):
     code = sp.lib.sp_tree_accept(P, P + 4096, P + 2 * 4096, None, 2, 4, P + 16, 2 * P, 3 * P, at, at + 4 * away, P + 4 * 4096, 4 * P, 16, layers, ld, 2, 64, 0, None)
     assert code == sp.SP_ERR_INVALID_ARG
     assert ("outputs" if apart else "tails overlap") in sp.lib.sp_last_error().decode()
+
+
+def test_no_kernel_waits_for_the_lanes_that_happen_to_be_there():
+    """A barrier over __activemask() orders nothing that the compiler did not keep together by itself; that it did so cannot be tested by running."""
+    csrc = pathlib.Path(sp.binding.LIB_PATH).parent / "csrc"
+    assert not [f.name for f in csrc.iterdir() if f.suffix in (".cu", ".cuh") and "__activemask" in f.read_text()]
 
 
 def test_plain_tree_of_a_chain_is_causal_attention():
