@@ -114,7 +114,8 @@ def _load() -> ctypes.CDLL:
 lib = _load()
 
 # The launching entry points go through the native marshalling module: its case number (the order here) and the kind of every
-# argument, t / r contiguous / strided tensor or None, a address, i integer, d floating point.
+# argument, t / r contiguous / strided tensor or None, w / f contiguous int32 / float32 tensor or None, a address, i integer,
+# d floating point.
 _KINDS = (
     ("sp_rope_apply", "rriiiiidiia"),
     ("sp_rope_apply_pair", "riiriiriiidiia"),
@@ -127,10 +128,11 @@ _KINDS = (
     ("sp_pruned_decode_alibi", "tttatitttiittttiiidttti" "ia"),
     ("sp_pruned_decode_rope", "tttatitttiitdiiiidttia"),
     ("sp_pruned_decode_static", "tttatitttiiiiidttia"),
-    ("sp_pruned_decode_tree", "tttatitttittiiiiidttti" "ia"),
-    ("sp_sample_tokens", "riiitttttttia"),
-    ("sp_tree_accept", "ttttiitttttttiiiiiia"),
+    ("sp_pruned_decode_tree", "tttawittwiwwiiiiidtfti" "ia"),
+    ("sp_sample_tokens", "riiiffwffwfia"),
+    ("sp_tree_accept", "wwwwiiwwwttwwiiiiiia"),
 )
+_marshal.types(torch.int32, torch.float32)
 for _i, (_name, _kinds) in enumerate(_KINDS):
     _marshal.bind(_i, ctypes.cast(getattr(lib, _name), ctypes.c_void_p).value, _kinds)
 (_ROPE, _ROPE_PAIR, _PREFILL, _PREFILL_ALIBI, _PREFILL_ROPE, _SCORES, _TOPK, _DECODE, _DECODE_ALIBI, _DECODE_ROPE,
@@ -347,8 +349,9 @@ def sp_decode_tree_workspace_bytes(n_prompts: int, max_nodes: int, n_heads: int,
 def sp_pruned_decode_tree(q, k_cache, v_cache, lay: DeviceLayout, kept_idx, k: int, tail_k, tail_v, tail_len,
                           tail_cap: int, parent, n_nodes, scale: float, out, lse=None, ws=None, max_keys: int = 0,
                           stream=None):
-    """Attention of a tree of drafted tokens: q, out [B, N, H, D], parent int32 [B, N], n_nodes int32 [B] or None; the
-    nodes' K / V are the tail rows behind the tail_len committed ones."""
+    """Attention of a tree of drafted tokens: q, out [B, N, H, D], kept_idx int32 [B, k], tail_len int32 [B], parent int32
+    [B, N], n_nodes int32 [B] or None, lse fp32 [B, N, H] or None; the nodes' K / V are the tail rows behind the tail_len
+    committed ones."""
     B, N, H, D = q.shape
     Hkv = k_cache.shape[1]
     _call(_DECODE_TREE, q, k_cache, v_cache, ctypes.addressof(lay.c), kept_idx, k, tail_k, tail_v, tail_len, tail_cap,
@@ -356,7 +359,8 @@ def sp_pruned_decode_tree(q, k_cache, v_cache, lay: DeviceLayout, kept_idx, k: i
 
 
 def sp_sample_tokens(logits, u, tokens, logp=None, *, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
-    """One token per row of logits [R, V] from uniform numbers u [R]; per-row settings are tensors [R] or None."""
+    """One token per row of logits [R, V] from uniform numbers u fp32 [R]; per-row settings are tensors [R] or None: top_k
+    int32, the others fp32.  tokens int32 [R], logp fp32 [R] or None."""
     R, V = logits.shape
     if R > 0 and V > 1 and logits.stride(1) != 1:
         raise ValueError("logits: the elements of a row must lie side by side")
@@ -366,21 +370,25 @@ def sp_sample_tokens(logits, u, tokens, logp=None, *, temperature=None, top_k=No
 
 def sp_tree_accept(draft, sampled, parent, n_nodes, path, n_accepted, next_token, tail_k=None, tail_v=None,
                    tail_len=None, new_tail_len=None, stream=None):
-    """The walk down a tree of drafts (draft, sampled, parent int32 [B, N]) and the compaction of the tails
+    """The walk down a tree of drafts (draft, sampled, parent, path int32 [B, N], the others int32 [B]) and the compaction of the tails
     [n_layers, slots, cap, Hkv, D] in place; prompt b has slot b, of B or more."""
     B, N = parent.shape
-    L, cap, ld, Hkv, D, dtype = 0, 0, 0, 0, 0, SP_F32
-    if (tail_k is None) != (tail_v is None):
-        raise ValueError("tail_k and tail_v come together")
-    if tail_k is not None:
-        if tail_v.shape != tail_k.shape or tail_v.dtype != tail_k.dtype:
+    if tail_k is None:
+        if tail_v is not None:
+            raise ValueError("tail_k and tail_v come together")
+        L = cap = ld = Hkv = D = dtype = 0
+    else:
+        if tail_v is None:
+            raise ValueError("tail_k and tail_v come together")
+        shape = tail_k.shape
+        L, slots, cap, Hkv, D = shape
+        if tail_v.shape != shape or tail_v.dtype is not tail_k.dtype:
             raise ValueError("tail_k and tail_v must have one shape and type")
-        L, slots, cap, Hkv, D = tail_k.shape
         if slots < B:
             raise ValueError(f"tails of {slots} slots for {B} prompts")
-        ld, dtype = tail_k.stride(0), dtype_code(tail_k)
-    _call(_ACCEPT, draft, sampled, parent, n_nodes, B, N, path, n_accepted, next_token, tail_k, tail_v, tail_len,
-          new_tail_len, cap, L, ld, Hkv, D, dtype, _stream(stream))
+        ld, dtype = slots * cap * Hkv * D, dtype_code(tail_k)
+    _check(_marshal.call(_ACCEPT, draft, sampled, parent, n_nodes, B, N, path, n_accepted, next_token, tail_k, tail_v,
+                         tail_len, new_tail_len, cap, L, ld, Hkv, D, dtype, _stream(stream)))
 
 
 def sp_check_status(ws, stream=None) -> None:

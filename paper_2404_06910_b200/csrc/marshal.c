@@ -3,8 +3,8 @@
  * Converting a decode step's twenty arguments with ctypes and reading a dozen tensors' addresses from Python took as long as
  * the launch itself (host time of a decode call 9.0 us, 6.1 through this module; a prefill call 15.1 and 7.8).  Here a tensor
  * costs two method calls and a number a conversion.
- * bind() receives the addresses of the library's entry points, call(index, ...) the arguments in the order of sp.h:
- * tensors (or None) for pointers, numbers otherwise.  What the arguments mean is checked by the library. */
+ * types() receives the element types that kinds w and f require, bind() the addresses of the library's entry points,
+ * call(index, ...) the arguments in the order of sp.h: tensors (or None) for pointers, numbers otherwise.  What the arguments mean is checked by the library. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -17,14 +17,24 @@
 typedef union { void *p; long long q; double d; } val;
 
 static struct { void *fn; char kinds[MAX_ARG + 1]; } entry[MAX_FN];
-static PyObject *s_data_ptr, *s_is_contiguous;
+static PyObject *s_data_ptr, *s_is_contiguous, *s_dtype, *dt_int32, *dt_float32;
 
-/* kinds: t contiguous tensor or None, r tensor as it is (strided), a address, i integer, d floating point */
+/* kinds: t contiguous tensor or None, w and f the same of int32 and float32, r tensor as it is (strided), a address, i integer,
+ * d floating point */
 static int convert(char kind, PyObject *o, val *v)
 {
-    if (kind == 't' || kind == 'r') {
+    if (kind == 't' || kind == 'w' || kind == 'f' || kind == 'r') {
         if (o == Py_None) { v->p = NULL; return 0; }
-        if (kind == 't') {
+        if (kind == 'w' || kind == 'f') {
+            PyObject *d = PyObject_GetAttr(o, s_dtype);
+            if (!d) return -1;
+            Py_DECREF(d);                        /* a type object lives on */
+            if (d != (kind == 'w' ? dt_int32 : dt_float32)) {
+                PyErr_Format(PyExc_TypeError, "a tensor of %R where %R is required", d, kind == 'w' ? dt_int32 : dt_float32);
+                return -1;
+            }
+        }
+        if (kind != 'r') {
             PyObject *c = PyObject_CallMethodNoArgs(o, s_is_contiguous);
             if (!c) return -1;
             const int yes = c == Py_True;
@@ -56,6 +66,15 @@ static PyObject *bind(PyObject *self, PyObject *args)
     entry[i].fn = PyLong_AsVoidPtr(address);
     strcpy(entry[i].kinds, kinds);
     if (PyErr_Occurred()) return NULL;
+    Py_RETURN_NONE;
+}
+
+static PyObject *types(PyObject *self, PyObject *args)
+{
+    (void)self;
+    if (!PyArg_ParseTuple(args, "OO", &dt_int32, &dt_float32)) return NULL;
+    Py_INCREF(dt_int32);
+    Py_INCREF(dt_float32);
     Py_RETURN_NONE;
 }
 
@@ -142,6 +161,7 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
 
 static PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, "bind(index, address, kinds)"},
+    {"types", types, METH_VARARGS, "types(int32, float32): what tensors of kinds w and f must be of"},
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call(index, *arguments) -> status"},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -150,5 +170,6 @@ PyMODINIT_FUNC PyInit__marshal(void)
 {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-    return s_data_ptr && s_is_contiguous ? PyModule_Create(&module) : NULL;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    return s_data_ptr && s_is_contiguous && s_dtype ? PyModule_Create(&module) : NULL;
 }

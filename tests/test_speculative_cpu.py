@@ -110,6 +110,37 @@ def test_accept_refuses_k_and_v_tails_that_overlap(layers, ld, away, apart):
     assert ("outputs" if apart else "tails overlap") in sp.lib.sp_last_error().decode()
 
 
+def _call_with(name, **types):
+    """A call of the front end that has nothing to do, with tensors of the given types in place of int32 and fp32."""
+    i32 = lambda n, *s: torch.zeros(s, dtype=types.get(n, torch.int32))
+    f32 = lambda n, *s: torch.zeros(s, dtype=types.get(n, torch.float32))
+    stream = SimpleNamespace(cuda_stream=0)
+    if name == "tree":
+        x, lay = torch.zeros(1, 0, 4, 64), sp.DeviceLayout.from_host(build_layout([2], [[2]], [[1]]), "cpu")
+        tail = torch.zeros(1, 4, 4, 64)
+        sp.sp_pruned_decode_tree(x, tail[0], tail[0], lay, i32("kept_idx", 1, 1), 1, tail, tail, i32("tail_len", 1), 4, i32("parent", 1, 0), i32("n_nodes", 1), 0.1, x, f32("lse", 1, 0, 4),
+                                 torch.zeros(256, dtype=torch.uint8), stream=stream)
+    elif name == "sample":
+        sp.sp_sample_tokens(torch.zeros(0, 8), f32("u", 0), i32("tokens", 0), f32("logp", 0), temperature=f32("temperature", 0), top_k=i32("top_k", 0), top_p=f32("top_p", 0),
+                            min_p=f32("min_p", 0), stream=stream)
+    else:
+        tree = lambda n: i32(n, 0, 4)
+        sp.sp_tree_accept(tree("draft"), tree("sampled"), tree("parent"), i32("n_nodes", 0), tree("path"), i32("n_accepted", 0), i32("next_token", 0), torch.zeros(1, 0, 8, 2, 64),
+                          torch.zeros(1, 0, 8, 2, 64), i32("tail_len", 0), i32("new_tail_len", 0), stream=stream)
+
+
+@pytest.mark.parametrize("name,arguments", [
+    ("tree", ["kept_idx", "tail_len", "parent", "n_nodes", "lse"]), ("sample", ["u", "tokens", "logp", "temperature", "top_k", "top_p", "min_p"]),
+    ("accept", ["draft", "sampled", "parent", "n_nodes", "path", "n_accepted", "next_token", "tail_len", "new_tail_len"])])
+def test_tensors_of_other_types_are_refused(name, arguments):
+    """Whole numbers are int64 and reals fp32 or fp64 where nobody says otherwise: not to be read as if they were int32 and fp32."""
+    _call_with(name)
+    for a in arguments:
+        for wrong in (torch.int64, torch.float64, torch.float32 if a not in ("u", "logp", "lse", "temperature", "top_p", "min_p") else torch.int32):
+            with pytest.raises(TypeError, match="int32|float32"):
+                _call_with(name, **{a: wrong})
+
+
 def test_no_kernel_waits_for_the_lanes_that_happen_to_be_there():
     """A barrier over __activemask() orders nothing that the compiler did not keep together by itself; that it did so cannot be tested by running."""
     csrc = pathlib.Path(sp.binding.LIB_PATH).parent / "csrc"
