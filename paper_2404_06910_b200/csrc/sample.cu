@@ -264,7 +264,7 @@ template <typename T, bool CLUSTER> struct Sampler {
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(exponent));
         return w;
     }
-    static constexpr double kOffPerExponent = 3 * 0x1p-24 * 0.6931471805599453 * 1.1, kOff = (0x1p-22 + 3 * 0x1p-24) * 1.1;
+    static constexpr double kOffPerExponent = 3 * 0x1p-24 * 0.6931471805599453 * 1.1, kOffAdded = 3 * 0x1p-24 * 1.1, kOff = 0x1p-22 * 1.1 + kOffAdded;
 
     // f(piece's four words, index of its first element) for this thread's pieces, which lie together, so that threads are in index order; an odd
     // number of them each, so that eight neighbours' pieces meet no bank twice.
@@ -629,11 +629,18 @@ template <typename T, bool CLUSTER> struct Sampler {
         return found;
     }
     // What the difference of a partial sum and `share` of the total may be off by, if the partial sum is off by `part` and the total by `all`: (1 -
-    // share) of the first error and share of the rest's; a unit for each element, for the exact sums' own roundings.
+    // share) of the first error and share of the rest's, as the total's terms are the partial sum's too; a unit for each element, for the exact
+    // sums' own roundings.
     __device__ __forceinline__ u64 doubt(double share, u64 part, u64 all) const
     {
         const double p = (double)part, rest = fmax((double)all - p, 0.0);
         return (u64)(((1.0 - share) * p + share * rest) * 1.001) + a.vocab;
+    }
+    // The same where the two sums are of two passes: the elements' weights are alike in both, but not the additions in pieces of which only one
+    // pass takes all elements, nor the units that the threads' sums are cut to.
+    __device__ __forceinline__ u64 doubt_apart(double share, const Sum &part, const Sum &all) const
+    {
+        return doubt(share, part.off, all.off) + (u64)(((double)part.units + share * (double)all.units) * kOffAdded) + 2 * kSmpThreads * blocks();
     }
     // Where the elements' weights, in the order of the filters, reach goal, which is `share` of `all`, found among those down to `low`.  Threshold and last
     // index.  0: found, 1: not there, or too many elements lie there for the list, 2: not certain where in the list, which is sorted: n elements, the largest
@@ -690,7 +697,7 @@ template <typename T, bool CLUSTER> struct Sampler {
         n = join_list();
         if (n == 0 || n > kSmpList) return 1;
         sort(n);
-        return settle(n, part.units, goal, doubt(share, part.off, all.off), least, tie_last);
+        return settle(n, part.units, goal, doubt_apart(share, part, all), least, tie_last);
     }
     // The token, by one thread of the row.
     __device__ __forceinline__ void write(int64_t r, float x, int index, float temperature, u64 total) const
