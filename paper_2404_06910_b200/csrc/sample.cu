@@ -949,7 +949,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const __grid_con
         const u64 goal = min((u64)((double)u * (double)total), total - 1);
         if (!s.exact) part_off = s.row_scan(mine.off, all_off);
         s.find_thread(mine.units, upto, goal);
-        if ((int)threadIdx.x == sh.winner) sh.above = part_off;
+        if ((int)threadIdx.x == sh.winner) sh.above = part_off - mine.off;         // of the sums in front: the winner's own elements are weighed exactly below
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
         if (sh.winner >= 0 && threadIdx.x < 32) {
