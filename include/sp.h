@@ -329,7 +329,8 @@ int sp_pruned_decode_static(const void *q, const void *k_cache, const void *v_ca
  * they are.  k_cache, v_cache, lay, kept_idx, k and max_keys (nodes counted) as for sp_pruned_decode; q and K come
  * rotated (sp_rope_apply_pair).  A prompt whose n_nodes is not in [0, max_nodes], whose tail_len + n_nodes is not in
  * [0, tail_cap] or one of whose parents is not in [-1, node) is left out and reported (SP_ERR_LAYOUT from
- * sp_check_status).  head_dim in {64, 128}.  Softmax statistics and sums are fp32.
+ * sp_check_status); so is a preamble or kept path that the layout's arrays put outside the cache or make longer than
+ * max_pre_len / max_path_len.  head_dim in {64, 128}.  Softmax statistics and sums are fp32.
  * ws: at least sp_decode_tree_workspace_bytes() bytes, 256-byte aligned: the status word, written by every call.
  */
 size_t sp_decode_tree_workspace_bytes(int n_prompts, int max_nodes, int n_heads, int head_dim);

@@ -46,12 +46,40 @@ __device__ __forceinline__ bool tree_of_prompt(const TreeArgs &a, int b, int &n,
     return __all_sync(0xffffffffu, good);
 }
 
+// Segment s of prompt b (0: the preamble, then the kept paths): its first row in the cache and its length.  False where the layout's arrays put it outside
+// the cache or make it longer than the host was told: the segment is then empty and reported.  A kept index that is none of the prompt's paths is an
+// empty segment too, and fine, as in sp_pruned_decode.
+__device__ __forceinline__ bool tree_segment(const TreeArgs &a, int b, int s, int64_t &row, int64_t &len)
+{
+    int most = a.max_path_len;
+    bool good = true;
+    row = len = 0;
+    if (s == 0) {
+        row = a.pre_start[b]; len = a.pre_len[b]; most = a.max_pre_len;
+    } else {
+        const int i = a.kept_idx[(int64_t)b * a.k + s - 1], p0 = a.ppo[b], p1 = a.ppo[b + 1];
+        if (i >= max(p0, 0) && i < min(p1, a.n_paths)) {
+            const int doc = a.doc_len[i], qry = a.qry_len[i];
+            good = doc >= 0 && qry >= 0;
+            row = a.path_start[i]; len = (int64_t)doc + qry;
+        }
+    }
+    good = good && row >= 0 && len >= 0 && len <= most && row + len <= a.total_tokens;
+    if (!good) len = 0;
+    return good;
+}
+
 // The grid's first layer (z = 0; prompts follow) reports: it is scheduled before every other block, so that its plain store comes before any
-// other block could have something to add.  Kept paths that do not exist are skipped and not reported, as in sp_pruned_decode.
+// other block could have something to add.
 __device__ __forceinline__ void tree_report(const TreeArgs &a)
 {
     if (blockIdx.x || blockIdx.y) return;
     bool good = true;
+    const int64_t segments = (int64_t)a.n_prompts * (a.k + 1);
+    for (int64_t i = threadIdx.x; i < segments; i += blockDim.x) {
+        int64_t row, len;
+        good &= tree_segment(a, (int)(i / (a.k + 1)), (int)(i % (a.k + 1)), row, len);
+    }
     const int warps = blockDim.x / 32;
     for (int b = threadIdx.x >> 5; b < a.n_prompts; b += warps) {
         int n, committed, par[2];
@@ -102,17 +130,10 @@ struct TreeTable {
             }
             if (lane == 0) { head->n = n; head->committed = committed; head->good = good; }
         }
-        // lengths first, in end[] (a segment that the layout puts outside the cache is skipped); the first warp is busy with the tree
+        // lengths first, in end[]; the first warp is busy with the tree
         for (int s = (int)threadIdx.x - 32; threadIdx.x >= 32 && s < n_seg - 1; s += blockDim.x - 32) {
-            int64_t r = 0, len = 0;
-            int most = a.max_path_len;
-            if (s == 0) {
-                r = a.pre_start[b]; len = a.pre_len[b]; most = a.max_pre_len;
-            } else {
-                const int i = a.kept_idx[(int64_t)b * a.k + s - 1], p0 = a.ppo[b], p1 = a.ppo[b + 1];
-                if (i >= max(p0, 0) && i < min(p1, a.n_paths)) { r = a.path_start[i]; len = (int64_t)a.doc_len[i] + a.qry_len[i]; }
-            }
-            if (r < 0 || len < 0 || len > most || r + len > a.total_tokens) len = 0;
+            int64_t r, len;
+            tree_segment(a, b, s, r, len);
             row[s] = (int)r;
             end[s] = (int)len;
         }
