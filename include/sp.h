@@ -330,8 +330,11 @@ int sp_pruned_decode_static(const void *q, const void *k_cache, const void *v_ca
  * rotated (sp_rope_apply_pair).  A prompt whose n_nodes is not in [0, max_nodes], whose tail_len + n_nodes is not in
  * [0, tail_cap] or one of whose parents is not in [-1, node) is left out and reported (SP_ERR_LAYOUT from
  * sp_check_status); so is a preamble or kept path that the layout's arrays put outside the cache or make longer than
- * max_pre_len / max_path_len.  head_dim in {64, 128}.  Softmax statistics and sums are fp32.
- * ws: at least sp_decode_tree_workspace_bytes() bytes, 256-byte aligned: the status word, written by every call.
+ * max_pre_len / max_path_len.  head_dim in {64, 128}.  Softmax statistics and sums are fp32; with SP_BF16 the
+ * probabilities are multiplied with V as the sum of two bf16 numbers (16 bits), as in sp_pruned_decode.
+ * ws: at least sp_decode_tree_workspace_bytes() bytes, 256-byte aligned: the status word, written by every call that has
+ * prompts and nodes (one without leaves it as it is).  It is the last call's: layers that share a workspace overwrite
+ * one another's, so a step that looks at it once, at its end, has one workspace per layer.
  */
 size_t sp_decode_tree_workspace_bytes(int n_prompts, int max_nodes, int n_heads, int head_dim);
 int sp_pruned_decode_tree(const void *q, const void *k_cache, const void *v_cache, const sp_layout *lay,
@@ -354,8 +357,9 @@ int sp_pruned_decode_tree(const void *q, const void *k_cache, const void *v_cach
  * top_p, min_p: fp32 [n_rows], top_k: int32 [n_rows], each or NULL (1, 1, 0, 0); tokens: int32 [n_rows]; logp: fp32
  * [n_rows] or NULL.  vocab <= 262144.  The token is that of fp64 weights, rounded to multiples of 2^-44, and exact sums, so it
  * does not depend on the order of anything: rows are tried with fp32 weights and a bound on their sums' error, and sums
- * that leave a doubt are taken again exactly.  Of logp, W may be such a sum: relative error up to 2^-22 + 7 2^-24 + 3 2^-24
- * times the weighted mean of (max - x) / temperature.  No workspace.
+ * that leave a doubt are taken again exactly.  Of logp, W may be such a sum of fp32 weights: besides its own rounding logp
+ * is then off by up to 2^-22 + 7 2^-24 + 3 2^-24 times the weighted mean of (max - x) / temperature, an absolute error, which
+ * for a token with nearly all of the weight is more than the last bit of a logp near 0.  No workspace.
  */
 int sp_sample_tokens(const void *logits, int64_t ld_logits, int64_t n_rows, int vocab, const float *u,
                      const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,

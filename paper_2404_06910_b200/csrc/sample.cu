@@ -1,6 +1,6 @@
 // sp_sample_tokens: one token per row of logits, with temperature, top-k, top-p and min-p, from one given uniform number per row.
 //
-// A block (a cluster of two to eight where a row does not fit) holds its row in shared memory, so that the logits leave HBM once however many
+// A block (a cluster of two to eight where a row does not fit: see launch_sample) holds its row in shared memory, so that the logits leave HBM once however many
 // passes the filters take.
 // All three filters keep a prefix of one order (value descending, index ascending), so the kept set is a threshold value and the last index
 // among its ties; and the token is the first one in index order whose running sum of kept weights w = exp((x - max) / T) passes u W.
@@ -18,9 +18,10 @@
 // polynomial of degree 6, 1e-15), rounded once to multiples of 2^-44, and sums of 64-bit integers: exact, in any order, atomics included.  fp64
 // costs several times what fp32 does (a pass over 50432 elements by a block alone on its SM 3 and some 15 us), so rows are tried with fp32
 // weights and a bound on what their sums are off by; only sums that leave a doubt (in 1 to 2 rows of a hundred) are taken again, exactly.
-// Two rows share an SM.  What bounds a row is its chain of passes over shared memory (each some 4 us for two rows, by the exponentials' 16 per
-// clk) and of short steps of the whole block between barriers.  1024 bf16 rows of 50432, us (floor 16): greedy 33, nothing left out 76,
-// k = 20 59, k = 1000 141, p = 0.9 184, settings as requests have them 117.
+// Two rows share an SM where they fit (100 KB: 51 000 elements in bf16, 25 000 in fp32); a longer one has it to itself.  What bounds a row is its
+// chain of passes over shared memory (each some 4 us for two rows, by the exponentials' 16 per clk) and of short steps of the whole block between
+// barriers.  1024 bf16 rows of 50432, us with cold L2 (floor 16): greedy 33, nothing left out 76, k = 20 59, k = 1000 143, p = 0.9 199, settings as
+// requests have them 122; those of 65000: 174, of 128000, a cluster of two a row: 460.  256 fp32 rows of 32000, top-p and min-p: 64 (two waves).
 #include <cooperative_groups.h>
 
 #include <cfloat>
@@ -996,7 +997,10 @@ template <typename T> static int launch_sample(SampleArgs &a, int64_t rows, cuda
 {
     constexpr int N = Vec<T>::N;
     const size_t head = round_up(sizeof(SampleShared), 16);
-    // Blocks per row: one where two of them fit on an SM, else as many as make them fit, eight at most.
+    // Blocks per row: one as long as the row fits into its shared memory, whether or not that leaves room for a second block on the SM; else as many as it
+    // takes, eight at most.  (A cluster of two, so that two blocks share an SM again, costs the barriers of a cluster in every short step: 256 fp32 rows of
+    // 32000, top-p and min-p, 72 us with one block and 102 with two; 64 of them 47 and 61; without filters 37 and 43; 1024 bf16 rows of 65000, mixed, 174 and
+    // 225, of 80000 217 and 260; 64 bf16 rows of 65000, temperature only, 41 and 41.)
     int n = 1;
     const auto vecs = [&](int n) { return (a.vocab + N - 1 + N - 1 + n * N - 1) / (n * N); };          // a row may start anywhere in a piece
     while (n < 8 && head + (size_t)vecs(n) * 16 > kSmpMaxSmem) n *= 2;
