@@ -74,16 +74,19 @@ __device__ __forceinline__ bool tree_segment(const TreeArgs &a, int b, int s, in
 __device__ __forceinline__ void tree_report(const TreeArgs &a)
 {
     if (blockIdx.x || blockIdx.y) return;
+    // A thread takes segments and places of nodes one by one, whatever prompt they are of, several loads under way at a time: with thousands of prompts of few
+    // keys this block would otherwise be the last to end.
     bool good = true;
-    const int64_t segments = (int64_t)a.n_prompts * (a.k + 1);
-    for (int64_t i = threadIdx.x; i < segments; i += blockDim.x) {
+    const uint32_t per = a.k + 1, segments = (uint32_t)a.n_prompts * per, nodes = (uint32_t)a.n_prompts * a.max_nodes;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < segments; i += blockDim.x) {
         int64_t row, len;
-        good &= tree_segment(a, (int)(i / (a.k + 1)), (int)(i % (a.k + 1)), row, len);
+        good &= tree_segment(a, i / per, i % per, row, len);
     }
-    const int warps = blockDim.x / 32;
-    for (int b = threadIdx.x >> 5; b < a.n_prompts; b += warps) {
-        int n, committed, par[2];
-        good &= tree_of_prompt(a, b, n, committed, par);
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < nodes; i += blockDim.x) {
+        const int b = i / a.max_nodes, node = i % a.max_nodes, n = a.n_nodes ? a.n_nodes[b] : a.max_nodes, committed = a.tail_len[b], parent = a.parent[i];
+        good &= n >= 0 && n <= a.max_nodes && committed >= 0 && (int64_t)committed + n <= a.tail_cap && (node >= n || (parent >= -1 && parent < node));
     }
     good = __syncthreads_and(good);
     if (threadIdx.x == 0) *a.status = good ? STATUS_OK : STATUS_BAD_LAYOUT;
